@@ -143,7 +143,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int bl
             }
             for (int d = 1; d < per_row; d <<= 1) merge(top, l, __shfl_xor(top, d), __shfl_xor(l, d));
             sm[x] = top == MINUS_INF ? 0.f : top;
-            sl[x] = top == MINUS_INF ? 0.f : 1.f / l;
+            sl[x] = l == 0.f ? 0.f : 1.f / l;
         }
         __syncthreads();
 #pragma unroll 1
@@ -220,9 +220,9 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int bl
             y[1] = y[1] * mine + sy[w][e + 1] * theirs;
             top = now;
         }
-        const float linv = top == MINUS_INF ? 0.f : 1.f / l;
-        y[0] = top == MINUS_INF ? 0.f : y[0] * linv;
-        y[1] = top == MINUS_INF ? 0.f : y[1] * linv;
+        const float linv = l == 0.f ? 0.f : 1.f / l; // (a sum of NaN is not nothing)
+        y[0] = l == 0.f ? 0.f : y[0] * linv;
+        y[1] = l == 0.f ? 0.f : y[1] * linv;
         const int h = x / a.M, m = x - h * a.M;
         const size_t to = (size_t)(b * a.M + m) * a.ldo + (size_t)(hk * a.G + h) * a.o_head + e;
         if constexpr (sizeof(T) == 2) store_out<T, 2>(a, to, y);

@@ -550,7 +550,7 @@ __global__ __launch_bounds__(ATTN_WAVES * 64) void paged_attn_kernel(PagedAttnAr
                 l += sm_l[w][rt][c] * wt[w];
             }
             const int x = x0 + rt * 16 + c;
-            const float linv = top == MINUS_INF ? 0.f : 1.f / l;
+            const float linv = l == 0.f ? 0.f : 1.f / l; // (nothing seen: no sum.  Scores of NaN leave no maximum either, but a sum of NaN)
             if (wave == 0 && g == 0) {
                 fin_m[rt * 16 + c] = safe;
                 fin_l[rt * 16 + c] = linv;
@@ -569,7 +569,7 @@ __global__ __launch_bounds__(ATTN_WAVES * 64) void paged_attn_kernel(PagedAttnAr
                         y[e] = 0.f;
 #pragma unroll
                         for (int w = 0; w < NW; ++w) y[e] += merge_at(w, cg * S::VE + e0 + e, r) * wt[w];
-                        if (whole) y[e] = top == MINUS_INF ? 0.f : y[e] * linv;
+                        if (whole) y[e] = l == 0.f ? 0.f : y[e] * linv;
                     }
                     const int at = cg * 16 * S::VE + S::VE * (4 * g + r) + e0;
                     if (whole) {

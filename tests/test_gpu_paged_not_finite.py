@@ -1,0 +1,66 @@
+"""ss_paged_attention of rows whose scores are no numbers: NaN comes out, and only where such a score was seen."""
+import pytest
+import torch
+
+import paper_2311_04951_amd as sv
+from paged_util import Cache
+
+pytestmark = pytest.mark.gpu
+
+NAN, INF = float("nan"), float("inf")
+# one launch | two: a workgroup to a head, equal parts that end inside heads; (lengths, query heads over two key heads, new rows, bound)
+FORMS = {"one launch": ([0, 37, 250], 2, 1, 251), "one launch, shared": ([0, 37, 240], 8, 4, 244), "joined": ([0, 37, 900], 2, 1, 0), "joined, shared": ([0, 37, 3000], 8, 4, 0),
+         "joined, many rows": ([0, 37, 700], 10, 5, 0), "one launch, many rows": ([0, 37, 100], 10, 5, 105)}
+
+
+def setup(seed, dtype, form):
+    lengths, heads, M, bound = FORMS[form]
+    c = Cache(seed, dtype, len(lengths), 2, 64, 16, lengths, room=M)
+    q = torch.randn((len(lengths), M, heads, 64), generator=c.generator).mul_(1.5).to(c.dtype)
+    return c, q, bound
+
+
+def attend(c, q, bound, weights):
+    kv = c.device()
+    w = torch.zeros(c.weight.shape, device="cuda") if weights else None
+    return sv.ss_paged_attention(kv, 0, q.cuda(), weight_out=w, max_len=bound).cpu(), w.cpu() if weights else None
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("weights", [False, True])
+@pytest.mark.parametrize("form", FORMS)
+def test_a_query_of_nan(dtype, weights, form):
+    """One element of one row: that row alone is NaN, whatever it sees (one position, some, all pieces of a long head)."""
+    c, q, bound = setup(1, dtype, form)
+    clean, _ = attend(c, q, bound, weights)
+    for b in range(q.shape[0]):
+        for m in {0, q.shape[1] - 1}:
+            for h in (0, q.shape[2] - 1):
+                dirty = q.clone()
+                dirty[b, m, h, 5] = NAN
+                out, w = attend(c, dirty, bound, weights)
+                assert out[b, m, h].isnan().all()
+                rest = torch.ones(q.shape[:3], dtype=torch.bool)
+                rest[b, m, h] = False
+                assert torch.equal(out[rest], clean[rest])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("weights", [False, True])
+@pytest.mark.parametrize("form", ["one launch", "joined"])
+def test_keys_of_nan(dtype, weights, form):
+    """All that a row sees: its own first position; a whole sequence; NaN beside scores of minus infinity.  Nothing but minus infinity: zero."""
+    c, q, bound = setup(2, dtype, form)
+    q[..., 0] = q[..., 0].abs() + 0.5
+    n = c.lengths
+    at = lambda b, s: (0, c.table[b, s // 16].long(), slice(None), s % 16)
+    c.k[at(0, torch.tensor([0]))] = NAN
+    c.k[at(1, torch.arange(n[1] + 1))] = NAN
+    c.k[at(2, torch.arange(n[2] + 1))] = 1.0
+    lowest = (0, c.table[2, torch.arange(n[2] + 1) // 16].long(), slice(None), torch.arange(n[2] + 1) % 16, 0)
+    c.k[lowest] = -INF                                   # scores of sequence 2: all minus infinity
+    out, _ = attend(c, q, bound, weights)
+    assert out[0].isnan().all() and out[1].isnan().all() and (out[2] == 0).all()
+    c.k[at(2, torch.tensor([n[2] // 2]))] = NAN          # ... but one
+    out, _ = attend(c, q, bound, weights)
+    assert out.isnan().all()
