@@ -161,6 +161,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int bl
                     load_scores(a, head, s, x, FIRST_STEP, t);
                     sum_scores(a, x, FIRST_STEP, sm, sl, t, sum);
                 }
+                sum_seen(a, head, s, n, x0, FIRST_STEP, sm, sl, sum);
             }
             if constexpr (BY_ROW) {
                 if (wave) quarter[wave - 1][lane] = sum;

@@ -223,6 +223,21 @@ __device__ __forceinline__ void sum_scores(const PagedAttnArgs &a, int first, in
             for (int i = 0; i < 4; ++i) sum[i] += exp2_(fmaf(t.v[j][i], a.scale_log2e, -top)) * l;
         }
 }
+// A row takes nothing from a slot that it does not see, a row of NaN neither, although a weight of zero times its reciprocal sum is NaN: where a sum
+// of the newest slots is NaN, it is made again without what is hidden.
+__device__ __forceinline__ void sum_seen(const PagedAttnArgs &a, int head, int s, int n, int first, int step, const float *m, const float *linv, f32x4 &sum) {
+    const int over = s + 3 - (n - a.M); // slots of the four behind the last that every row sees
+    if (over <= 0 || !(isnan(sum[0]) || isnan(sum[1]) || isnan(sum[2]) || isnan(sum[3]))) return;
+    sum = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int x = first; x < a.GM; x += step) {
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(a.scores + ((size_t)head * a.GM + x) * a.ld_scores + s);
+        const int last = 3 - over + x % a.M; // of the four, that the row sees
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i <= last) sum[i] += exp2_(fmaf(v[i], a.scale_log2e, -m[x])) * linv[x];
+    }
+}
 // Where slots s .. s + 3 keep their weights (they are in one page); -1: nowhere
 __device__ __forceinline__ int64_t weights_at(const PagedArgs &kv, int b, int hk, int s) {
     const int page = kv.table[(size_t)b * kv.max_pages + (s >> kv.page_bits)];
@@ -595,6 +610,7 @@ __global__ __launch_bounds__(ATTN_WAVES * 64) void paged_attn_kernel(PagedAttnAr
                     load_scores(a, b * kv.Hk + hk, s, x, 1, t);
                     sum_scores(a, x, 1, fin_m, fin_l, t, sum);
                 }
+                sum_seen(a, b * kv.Hk + hk, s, n, 0, 1, fin_m, fin_l, sum);
                 add_weights(a, at, s, n, old, sum);
             }
         if (WHOLE || !more) return;

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_2311_04951_amd as sv
-from paged_util import Cache
+from paged_util import Cache, attention64
 
 pytestmark = pytest.mark.gpu
 
@@ -64,3 +64,24 @@ def test_keys_of_nan(dtype, weights, form):
     c.k[at(2, torch.tensor([n[2] // 2]))] = NAN          # ... but one
     out, _ = attend(c, q, bound, weights)
     assert out.isnan().all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("form", ["one launch, shared", "joined, shared", "one launch, many rows", "joined, many rows"])
+@pytest.mark.parametrize("m", [0, 2])
+@pytest.mark.parametrize("bad", [NAN, INF])
+def test_a_row_of_nan_gives_nothing_to_what_it_does_not_see(dtype, form, m, bad):
+    """The newest positions, hidden from row m, hold what the rows behind it gave them; the others of its key head NaN; other heads' are as ever."""
+    c, q, bound = setup(3, dtype, form)
+    c.k[..., 5] = c.k[..., 5].abs() + 0.5                # (all scores of an infinite query are plus infinity)
+    M, last = q.shape[1], q.shape[2] - 1
+    _, gave, _ = attention64(c, 0, q, M)
+    q[:, m, last, 5] = bad
+    _, w = attend(c, q, bound, True)
+    for (b, h), (got, off) in gave.items():
+        s = torch.arange(len(got))
+        at = (0, c.table[b, s // 16].long(), h, s % 16)
+        have, want = w[at].double(), c.weight[at].double() + got
+        hidden = len(got) - M + m + 1 if h == 1 else 0       # the first slot that row m does not see
+        assert have[:hidden].isnan().all()
+        assert ((have - want).abs() <= off + want * 2.0 ** -23)[hidden:].all()
