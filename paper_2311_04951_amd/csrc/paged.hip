@@ -120,9 +120,9 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int bl
     // a head's pieces: parts first .. first + count - 1; the first one's is its last piece
     const int from = before * kv.Hk + hk * nb, first = from / share, count = (from + nb - 1) / share - first + 1;
     auto row_at = [&](int j, int x) { return ((size_t)(x / rows * a.workgroups + first + j) * 2 + (j == 0 ? 1 : 0)) * rows + x % rows; };
-    auto merge = [](float &top, float &l, float other, float other_l) {
+    auto merge = [&](float &top, float &l, float other, float other_l) {
         const float now = fmaxf(top, other), safe = now == MINUS_INF ? 0.f : now;
-        l = l * exp2_(top - safe) + other_l * exp2_(other - safe);
+        l = l * weight_of(top, safe, a.scale_log2e) + other_l * weight_of(other, safe, a.scale_log2e);
         top = now;
     };
     if (weights) {
@@ -143,7 +143,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int bl
             }
             for (int d = 1; d < per_row; d <<= 1) merge(top, l, __shfl_xor(top, d), __shfl_xor(l, d));
             sm[x] = top == MINUS_INF ? 0.f : top;
-            sl[x] = l == 0.f ? 0.f : 1.f / l;
+            sl[x] = saw_nothing(top, l) ? 0.f : 1.f / l;
         }
         __syncthreads();
 #pragma unroll 1
@@ -192,7 +192,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int bl
     #pragma unroll
             for (int d = 1; d < 8; d <<= 1) now = fmaxf(now, __shfl_xor(now, d));
             now = fmaxf(top, __shfl(now, 0));
-            const float safe = now == MINUS_INF ? 0.f : now, alpha = exp2_(top - safe), f = exp2_(ml.x - safe);
+            const float safe = now == MINUS_INF ? 0.f : now, alpha = weight_of(top, safe, a.scale_log2e), f = weight_of(ml.x, safe, a.scale_log2e);
             top = now;
             y[0] *= alpha;
             y[1] *= alpha;
@@ -215,15 +215,16 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int bl
         if (wave == 0 && e < kv.hd) {
     #pragma unroll
         for (int w = 1; w < 4; ++w) {
-            const float now = fmaxf(top, st[w][0]), safe = now == MINUS_INF ? 0.f : now, mine = exp2_(top - safe), theirs = exp2_(st[w][0] - safe);
+            const float now = fmaxf(top, st[w][0]), safe = now == MINUS_INF ? 0.f : now, mine = weight_of(top, safe, a.scale_log2e), theirs = weight_of(st[w][0], safe, a.scale_log2e);
             l = l * mine + st[w][1] * theirs;
             y[0] = y[0] * mine + sy[w][e] * theirs;
             y[1] = y[1] * mine + sy[w][e + 1] * theirs;
             top = now;
         }
-        const float linv = l == 0.f ? 0.f : 1.f / l; // (a sum of NaN is not nothing)
-        y[0] = l == 0.f ? 0.f : y[0] * linv;
-        y[1] = l == 0.f ? 0.f : y[1] * linv;
+        const bool nothing = saw_nothing(top, l);
+        const float linv = nothing ? 0.f : 1.f / l;
+        y[0] = nothing ? 0.f : y[0] * linv;
+        y[1] = nothing ? 0.f : y[1] * linv;
         const int h = x / a.M, m = x - h * a.M;
         const size_t to = (size_t)(b * a.M + m) * a.ldo + (size_t)(hk * a.G + h) * a.o_head + e;
         if constexpr (sizeof(T) == 2) store_out<T, 2>(a, to, y);

@@ -46,9 +46,9 @@ struct PagedAttnArgs {
     int stream;        // ask for keys and values with the non-temporal bit
     // set by the launcher
     int rowblocks, row_tiles, workgroups; // workgroups: parts of the positions, each of a workgroup to a block of rows
-    float2 *part_ml; // [rowblocks][2 * workgroups][16 * row_tiles] running maximum (log2 domain) and sum of a piece
+    float2 *part_ml; // [rowblocks][2 * workgroups][16 * row_tiles] largest score and sum of weights of a piece
     float *part_o;   // [rowblocks][2 * workgroups][16 * row_tiles][hd] unnormalised
-    float2 *row_stats; // [B*Hk*GM] maximum and reciprocal sum of the rows of units that one workgroup had (with weights and several row blocks)
+    float2 *row_stats; // [B*Hk*GM] largest score and reciprocal sum of weights of the rows of units that one workgroup had (with weights and several row blocks)
     float *scores;   // [B*Hk*GM][ld_scores] products of queries and keys
     int64_t ld_scores;
 };

@@ -85,3 +85,25 @@ def test_a_row_of_nan_gives_nothing_to_what_it_does_not_see(dtype, form, m, bad)
         hidden = len(got) - M + m + 1 if h == 1 else 0       # the first slot that row m does not see
         assert have[:hidden].isnan().all()
         assert ((have - want).abs() <= off + want * 2.0 ** -23)[hidden:].all()
+
+
+@pytest.mark.parametrize("weights", [False, True])
+@pytest.mark.parametrize("form", ["one launch", "joined"])
+def test_equal_scores_of_any_size(weights, form):
+    """All scores of a row equal, from 2^20 to 2^100 either way: the mean of the values, and equal weights."""
+    c, q, bound = setup(4, "f32", form)
+    for power in range(20, 101):
+        for sign in (1.0, -1.0):
+            q[:] = 1.37 * 2.0 ** (power - 20)
+            c.k[:] = sign * 1.13 * 2.0 ** 17             # 64 products times 1/8
+            out, w = attend(c, q, bound, weights)
+            for b, n in enumerate(c.lengths):
+                s = torch.arange(n + 1)
+                for h in range(2):
+                    mean = c.rows(c.v, 0, b, h, n + 1).double().mean(0)
+                    # values are at most 5; as many additions as there are positions
+                    assert ((out[b, 0, h].double() - mean).abs() <= (n + 64) * 2.0 ** -24 * 5).all(), (power, sign, b, h)
+                    if weights:
+                        at = (0, c.table[b, s // 16].long(), h, s % 16)
+                        want = c.weight[at].double() + 1 / (n + 1)
+                        assert ((w[at].double() - want).abs() <= want * (n + 64) * 2.0 ** -24).all(), (power, sign, b, h)
