@@ -8,6 +8,7 @@
 
 #include <cmath>
 #include <cstdarg>
+#include <limits>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -1538,7 +1539,7 @@ extern "C" int ss_paged_attention(const ss_paged_kv *kv, int32_t layer, const vo
     a.weight_out = weight_out_dev ? weight_out_dev + (a.kv.weight - kv->weight) : nullptr;
     a.H = n_heads; a.G = n_heads / kv->n_kv_heads; a.M = M; a.GM = a.G * M;
     a.pending = pending; a.max_n = bound;
-    a.scale_log2e = std::max((float)(1.4426950408889634 * std::fabs(scale)), 1e-30f); // (of a scale of 0: as good as 0 for every finite score)
+    a.scale_log2e = std::max((float)(1.4426950408889634 * std::fabs(scale)), std::numeric_limits<float>::denorm_min()); // (0 times a hidden score of minus infinity would be NaN)
     a.turn = scale < 0;
     launch_paged_attention(kv->dtype, a, ws_dev, (hipStream_t)stream);
     return check_launch();

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_2311_04951_amd as sv
-from paged_util import Cache, attention64
+from paged_util import Cache, attention64, check_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -107,3 +107,18 @@ def test_equal_scores_of_any_size(weights, form):
                         at = (0, c.table[b, s // 16].long(), h, s % 16)
                         want = c.weight[at].double() + 1 / (n + 1)
                         assert ((w[at].double() - want).abs() <= want * (n + 64) * 2.0 ** -24).all(), (power, sign, b, h)
+
+
+@pytest.mark.parametrize("weights", [False, True])
+@pytest.mark.parametrize("form", ["one launch, shared", "joined, shared"])
+@pytest.mark.parametrize("scale,size", [(0.0, 1.0), (0.0, 1e18), (-0.0, 1e18), (1e-36, 1e18), (-3e-34, 1e17)])
+def test_scales_next_to_zero(weights, form, scale, size):
+    """Of products up to 1e37 a scale of zero makes equal weights, one of 1e-36 those of the definition."""
+    c, q, bound = setup(5, "f32", form)
+    c.k *= size
+    q *= size
+    kv = c.device()
+    w = torch.full(c.weight.shape, 0.5, device="cuda") if weights else None
+    before = w.cpu().clone() if weights else None
+    out = sv.ss_paged_attention(kv, 0, q.cuda(), scale=scale, weight_out=w, max_len=bound)
+    check_attention(c, 0, q, q.shape[1], out, scale, w, before)
