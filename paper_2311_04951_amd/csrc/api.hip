@@ -1527,7 +1527,8 @@ extern "C" int ss_paged_attention(const ss_paged_kv *kv, int32_t layer, const vo
     if (((uintptr_t)q_dev & 15) || ((uintptr_t)out_dev & 15) || ld_q % E || head_q % E || ld_out % E || head_out % E)
         return fail(SS_EINVAL, "%s: queries, output and their strides must be multiples of 16 bytes", who);
     if (pending < 0) return fail(SS_EINVAL, "%s: pending %d", who, pending);
-    if (!std::isfinite(scale)) return fail(SS_EINVAL, "%s: the scale is not finite", who);
+    const float scale_log2e = (float)(1.4426950408889634 * std::fabs(scale));
+    if (!std::isfinite(scale_log2e)) return fail(SS_EINVAL, "%s: the scale, or its product with log2(e), is not finite", who);
     if ((uintptr_t)weight_out_dev & 15) return fail(SS_EINVAL, "%s: weights must be 16-byte aligned", who);
     if (weight_out_dev && !kv->weight) return fail(SS_EINVAL, "%s: weights asked for from a cache without them", who);
     const int bound = paged_bound(kv, max_len);
@@ -1539,7 +1540,7 @@ extern "C" int ss_paged_attention(const ss_paged_kv *kv, int32_t layer, const vo
     a.weight_out = weight_out_dev ? weight_out_dev + (a.kv.weight - kv->weight) : nullptr;
     a.H = n_heads; a.G = n_heads / kv->n_kv_heads; a.M = M; a.GM = a.G * M;
     a.pending = pending; a.max_n = bound;
-    a.scale_log2e = std::max((float)(1.4426950408889634 * std::fabs(scale)), std::numeric_limits<float>::denorm_min()); // (0 times a hidden score of minus infinity would be NaN)
+    a.scale_log2e = std::max(scale_log2e, std::numeric_limits<float>::denorm_min()); // (0 times a hidden score of minus infinity would be NaN)
     a.turn = scale < 0;
     launch_paged_attention(kv->dtype, a, ws_dev, (hipStream_t)stream);
     return check_launch();
