@@ -9,7 +9,9 @@ from __future__ import annotations
 
 import array
 import atexit
+import contextlib
 import functools
+import threading
 import weakref
 import ctypes as C
 import os
@@ -682,6 +684,16 @@ class PagedKV:
 
 
 _paged_workspaces = {}
+_paged_locks = {}
+_no_lock = contextlib.nullcontext()
+
+
+def _paged_lock(kv, ws, handle):
+    """What a call holds from the choice of its scratch until all of its launches are in the stream: a call is two launches, the second reads what the
+    first one left in the scratch, and another thread's call on the same stream would come between them."""
+    if ws is not None:
+        return _no_lock     # the caller's, of one call at a time
+    return _paged_locks.get((kv._device, handle)) or _paged_locks.setdefault((kv._device, handle), threading.Lock())
 
 
 def _paged_ws(kv, ws, key, need_of, handle):
@@ -756,11 +768,12 @@ def ss_paged_attention(kv: PagedKV, layer: int, q, out=None, pending=None, scale
         raise ValueError("weights asked for from a cache without them")
     w = _paged_like(kv, weight_out, kv.weight, "weights")
     stream = _stream(stream)
-    ws = _paged_ws(kv, ws, (n_heads, M, max_len, w is None), lambda: ss_paged_attention_workspace_bytes(kv, n_heads, M, max_len, w is not None),
-                   stream)
-    _check(lib().ss_paged_attention(kv._p, layer, *_paged_rows(kv, q, n_heads, "queries"), n_heads, M, M if pending is None else pending,
-                                    kv.head_dim ** -0.5 if scale is None else scale, *_paged_rows(kv, out, n_heads, "output"), w, max_len,
-                                    *ws, stream))
+    with _paged_lock(kv, ws, stream):
+        ws = _paged_ws(kv, ws, (n_heads, M, max_len, w is None), lambda: ss_paged_attention_workspace_bytes(kv, n_heads, M, max_len, w is not None),
+                       stream)
+        _check(lib().ss_paged_attention(kv._p, layer, *_paged_rows(kv, q, n_heads, "queries"), n_heads, M, M if pending is None else pending,
+                                        kv.head_dim ** -0.5 if scale is None else scale, *_paged_rows(kv, out, n_heads, "output"), w, max_len,
+                                        *ws, stream))
     return out
 
 
@@ -775,8 +788,9 @@ def ss_paged_evict(kv: PagedKV, budget: int, keep_first: int = 0, keep_recent: i
     out = (_paged_like(kv, weight_out, kv.weight, "weights"), _paged_like(kv, position_out, kv.position, "positions"),
            _paged_like(kv, len_out, kv.length, "lengths"))
     stream = _stream(stream)
-    ws = _paged_ws(kv, ws, (budget, max_len), lambda: ss_paged_evict_workspace_bytes(kv, budget, max_len), stream)
-    _check(lib().ss_paged_evict(kv._p, budget, keep_first, keep_recent, *out, max_len, *ws, stream))
+    with _paged_lock(kv, ws, stream):
+        ws = _paged_ws(kv, ws, (budget, max_len), lambda: ss_paged_evict_workspace_bytes(kv, budget, max_len), stream)
+        _check(lib().ss_paged_evict(kv._p, budget, keep_first, keep_recent, *out, max_len, *ws, stream))
 
 
 def ss_paged_forward_workspace_bytes(model: Model, kv: PagedKV, M: int, max_len: int = 0, weights: bool = False) -> int:
@@ -795,7 +809,8 @@ def ss_paged_forward(model: Model, kv: PagedKV, tokens, M: int, logits=None, wei
     lp = None if logits is False else logits
     stream = _stream(stream)
     key = ("forward", model.shape.n_heads, model.shape.head_dim, M, max_len, bool(weights))
-    ws = _paged_ws(kv, ws, key, lambda: ss_paged_forward_workspace_bytes(model, kv, M, max_len, weights), stream)
-    _check(lib().ss_paged_forward(model.handle, kv._p, _dev(tokens, torch.int32), M, int(bool(weights)), max_len,
-                                  _dev(lp, torch.float32 if lp is not None else None), *ws, stream))
+    with _paged_lock(kv, ws, stream):
+        ws = _paged_ws(kv, ws, key, lambda: ss_paged_forward_workspace_bytes(model, kv, M, max_len, weights), stream)
+        _check(lib().ss_paged_forward(model.handle, kv._p, _dev(tokens, torch.int32), M, int(bool(weights)), max_len,
+                                      _dev(lp, torch.float32 if lp is not None else None), *ws, stream))
     return lp
