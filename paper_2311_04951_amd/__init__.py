@@ -138,6 +138,7 @@ def lib():
             "ss_paged_forward": [vp, vp, vp, i32, i32, i32, vp, vp, sz, vp],
             "ss_paged_evict": [vp, i32, i32, i32, vp, vp, vp, i32, vp, sz, vp],
         }
+        L.hipStreamIsCapturing.argtypes = [vp, vp]      # (found in the HIP runtime that it is linked with)
         for name, args in sig.items():
             getattr(L, name).argtypes = args
         _lib = L
@@ -688,6 +689,13 @@ _paged_locks = {}
 _no_lock = contextlib.nullcontext()
 
 
+def _captures(handle):
+    """Whether the stream of this handle is being captured (the default stream cannot be).  Asked of the HIP runtime that the library runs on: torch tells
+    it of the current stream only, and making another one current and back costs 9 us."""
+    status = C.c_int(0)
+    return handle != 0 and lib().hipStreamIsCapturing(handle, C.byref(status)) == 0 and status.value != 0
+
+
 def _paged_lock(kv, ws, handle):
     """What a call holds from the choice of its scratch until all of its launches are in the stream: a call is two launches, the second reads what the
     first one left in the scratch, and another thread's call on the same stream would come between them."""
@@ -700,7 +708,7 @@ def _paged_ws(kv, ws, key, need_of, handle):
     """(address, bytes) of the scratch of a call on `kv`: the caller's, or one per (device, stream that the call runs on), kept between calls and
     replaced by a larger one when a call needs more - which a graph would not notice, so a call that is captured brings its own."""
     if ws is None:
-        if torch._C._cuda_isCurrentStreamCapturing():
+        if torch._C._cuda_isCurrentStreamCapturing() or _captures(handle):
             raise ValueError("a call that is captured into a graph needs a workspace of its own (ws=)")
         need = kv._ws.get(key)
         if need is None:

@@ -50,6 +50,7 @@ def library(monkeypatch):
     monkeypatch.setattr(sv, "lib", lambda: fake)
     monkeypatch.setattr(sv, "_stream", lambda stream: 0 if stream is None else stream)
     monkeypatch.setattr(torch._C, "_cuda_isCurrentStreamCapturing", lambda: False)
+    monkeypatch.setattr(sv, "_captures", lambda handle: False)
     # scratch that is there already: one for each of two streams
     monkeypatch.setattr(sv, "_paged_workspaces", {(torch.device("cpu"), h): torch.empty(1 << 22, dtype=torch.uint8) for h in (0, 1)})
     return fake
