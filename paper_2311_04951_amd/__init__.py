@@ -712,6 +712,8 @@ def _paged_ws(kv, ws, key, need_of, handle):
             raise ValueError("a call that is captured into a graph needs a workspace of its own (ws=)")
         need = kv._ws.get(key)
         if need is None:
+            if len(kv._ws) >= 256:      # (a loop whose bound grows by a position a token)
+                kv._ws.clear()
             need = kv._ws[key] = need_of()
         ws = _paged_workspaces.get((kv._device, handle))
         if ws is None or ws.numel() < need:

@@ -86,3 +86,16 @@ def test_a_call_that_fails_leaves_the_scratch_to_others(library):
     for _ in range(2):
         with pytest.raises(sv.SpecVerifyError):
             sv.ss_paged_attention(kv, 0, q)
+
+
+def test_what_a_cache_remembers_of_workspaces_is_bounded(library):
+    """A decoding loop passes another bound with every token."""
+    kv, q = cache(), torch.zeros(1, 1, 2, 64)
+    library.note = lambda ws, size: 0
+    for n in range(1, 1000):
+        sv.ss_paged_attention(kv, 0, q, max_len=n)
+        sv.ss_paged_evict(kv, 8, max_len=n)
+    assert len(kv._ws) <= 256
+    library.need = 1 << 20
+    sv.ss_paged_attention(kv, 0, q, max_len=999)             # (remembered)
+    assert max(kv._ws.values()) == 1 << 21
