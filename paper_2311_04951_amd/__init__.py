@@ -742,6 +742,8 @@ def _paged_rows(kv, t, heads, what):
 def _paged_like(kv, t, like, what):
     if t is None:
         return None
+    if like is None:
+        raise ValueError(f"{what} asked for from a cache without them")
     if t.shape != like.shape or t.device != like.device:
         raise ValueError(f"expected {what} of the cache's shape, on its device")
     return _dev(t, like.dtype)
@@ -769,13 +771,13 @@ def ss_paged_attention(kv: PagedKV, layer: int, q, out=None, pending=None, scale
     """q [batch, M, n_heads, head_dim] over the positions of one layer -> [batch, M, n_heads, head_dim].  pending: rows appended since
     the lengths moved (default: the call's own M); scale: default 1 / sqrt(head_dim); weight_out: kv.weight, or a tensor like it, to
     add up what every position receives; max_len: a bound on the positions of any sequence that the host knows."""
-    n_heads, M = q.shape[2] if q.dim() == 4 else 0, q.shape[1]
+    if q.dim() != 4:
+        raise ValueError("expected queries [batch, M, heads, head_dim]")
+    n_heads, M = q.shape[2], q.shape[1]
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     elif out.shape != q.shape:
         raise ValueError("queries and output of different shapes")
-    if weight_out is not None and kv.weight is None:
-        raise ValueError("weights asked for from a cache without them")
     w = _paged_like(kv, weight_out, kv.weight, "weights")
     stream = _stream(stream)
     with _paged_lock(kv, ws, stream):

@@ -99,3 +99,14 @@ def test_what_a_cache_remembers_of_workspaces_is_bounded(library):
     library.need = 1 << 20
     sv.ss_paged_attention(kv, 0, q, max_len=999)             # (remembered)
     assert max(kv._ws.values()) == 1 << 21
+
+
+def test_arguments_that_do_not_fit_are_refused_as_such(library):
+    kv, w = cache(), torch.zeros(1, 4, 2, 16)
+    with pytest.raises(ValueError, match="weights"):
+        sv.ss_paged_evict(kv, 8, weight_out=w)               # a cache without weights
+    with pytest.raises(ValueError, match="positions"):
+        sv.ss_paged_evict(kv, 8, position_out=w.int())
+    for shape in ((64,), (2, 64), (1, 2, 64)):
+        with pytest.raises(ValueError, match="queries"):
+            sv.ss_paged_attention(kv, 0, torch.zeros(shape))
