@@ -53,19 +53,21 @@ def budgeted_generate(target: Model, prompts, n_new: int, temperature: float, bu
                       page_size: int = 64, stats=None):
     """`prompts` (lists of token ids, any lengths from one token) are continued by n_new tokens each, all of them in one batch, with at
     most `budget` cached positions per head behind every eviction and a page more in front of it.  temperature 0: the most probable
-    token; else one drawn with the uniforms u [batch][n_new].  keep_recent: positions that are always kept (default: half the
-    budget).  Returns a list of token lists; `stats` (a dict, optional) receives evictions, pages (most in use) and loop_seconds."""
+    token; else one drawn with the uniforms u [batch][n_new].  keep_recent: positions that are always kept (0: half of what
+    keep_first leaves of the budget).  Returns a list of token lists; `stats` (a dict, optional) receives evictions, pages (most in use) and loop_seconds."""
     dev = torch.device("cuda")
     B, V = len(prompts), target.shape.vocab
     if not all(len(p) for p in prompts):
         raise ValueError("a prompt needs at least one token")
-    keep_recent = keep_recent or (budget - keep_first) // 2
+    if budget < 1 or keep_first < 0 or keep_recent < 0:
+        raise ValueError(f"budget {budget}, keep_first {keep_first}, keep_recent {keep_recent}")
+    keep_first = min(keep_first, budget)
+    keep_recent = min(keep_recent or (budget - keep_first) // 2, budget - keep_first)
     limit = budget + page_size                                        # where a sequence is brought back to its budget
     chunk = min(16, page_size, target.max_rows)
     pages = -(-limit // page_size)
     cache = PagedCache(target, B, B * pages, page_size, pages)
-    keep_first, everybody = min(keep_first, budget), range(B)
-    keep_recent = min(keep_recent, budget - keep_first)
+    everybody = range(B)
     evictions = used = 0
 
     def forward(kv, members, tokens, M, logits):

@@ -1,0 +1,15 @@
+"""What a decode loop over pages refuses before it begins, without a GPU."""
+import types
+
+import pytest
+
+import seeded_inputs as si
+from paper_2311_04951_amd.paged import budgeted_generate
+
+TARGET = types.SimpleNamespace(shape=si.TINY_TARGET, max_rows=16, max_pos=64)
+
+
+@pytest.mark.parametrize("changes", [dict(budget=0), dict(budget=-3), dict(keep_first=-1), dict(keep_recent=-2)])
+def test_budgets_that_keep_nothing(changes):
+    with pytest.raises(ValueError, match="budget"):
+        budgeted_generate(TARGET, [[1, 2]], 4, 0.0, **{"budget": 8, **changes})
