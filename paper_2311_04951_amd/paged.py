@@ -51,7 +51,7 @@ class PagedCache:
 
 def budgeted_generate(target: Model, prompts, n_new: int, temperature: float, budget: int, u=None, keep_first: int = 4, keep_recent: int = 0,
                       page_size: int = 64, stats=None):
-    """`prompts` (lists of token ids, any lengths from one token) are continued by n_new tokens each, all of them in one batch, with at
+    """`prompts` (lists of token ids, any lengths from one token, with n_new at most the model's max_pos + 1) are continued by n_new tokens each, all of them in one batch, with at
     most `budget` cached positions per head behind every eviction and a page more in front of it.  temperature 0: the most probable
     token; else one drawn with the uniforms u [batch][n_new].  keep_recent: positions that are always kept (0: half of what
     keep_first leaves of the budget).  Returns a list of token lists; `stats` (a dict, optional) receives evictions, pages (most in use) and loop_seconds."""
@@ -61,6 +61,9 @@ def budgeted_generate(target: Model, prompts, n_new: int, temperature: float, bu
         raise ValueError("a prompt needs at least one token")
     if budget < 1 or keep_first < 0 or keep_recent < 0:
         raise ValueError(f"budget {budget}, keep_first {keep_first}, keep_recent {keep_recent}")
+    last = max(len(p) for p in prompts) + n_new - 1                   # positions that the longest sequence feeds
+    if last > target.max_pos:
+        raise ValueError(f"{last} positions of a model whose rotary table has {target.max_pos}")
     keep_first = min(keep_first, budget)
     keep_recent = min(keep_recent or (budget - keep_first) // 2, budget - keep_first)
     limit = budget + page_size                                        # where a sequence is brought back to its budget

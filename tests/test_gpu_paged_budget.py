@@ -21,3 +21,10 @@ def test_budgets_of_a_few_positions(budget):
     got = budgeted_generate(gm, prompts, 40, 0.0, budget, page_size=16, stats=stats)
     assert stats["evictions"] >= 4 and all(len(g) == 40 for g in got)
     assert got == budgeted_generate(gm, prompts, 40, 0.0, budget, page_size=16)
+
+
+def test_up_to_the_models_last_position():
+    gm = model(10, 64)
+    for n, n_new in ((1, 64), (60, 5), (64, 1)):
+        prompt = si.token_ids(10, f"p{n}", (n,), si.TINY_TARGET.vocab).tolist()
+        assert len(budgeted_generate(gm, [prompt, prompt[:1]], n_new, 0.0, 24, page_size=16)[0]) == n_new

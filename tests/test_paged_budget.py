@@ -13,3 +13,10 @@ TARGET = types.SimpleNamespace(shape=si.TINY_TARGET, max_rows=16, max_pos=64)
 def test_budgets_that_keep_nothing(changes):
     with pytest.raises(ValueError, match="budget"):
         budgeted_generate(TARGET, [[1, 2]], 4, 0.0, **{"budget": 8, **changes})
+
+
+def test_generations_behind_the_rotary_table():
+    """A prompt of n tokens and n_new of them feed n + n_new - 1 positions; the model has 64."""
+    for n, n_new in ((1, 65), (60, 6), (65, 1), (66, 0), (400, 40)):
+        with pytest.raises(ValueError, match="rotary"):
+            budgeted_generate(TARGET, [[1, 2], [3] * n], n_new, 0.0, 8)
