@@ -64,6 +64,10 @@ def budgeted_generate(target: Model, prompts, n_new: int, temperature: float, bu
     last = max(len(p) for p in prompts) + n_new - 1                   # positions that the longest sequence feeds
     if last > target.max_pos:
         raise ValueError(f"{last} positions of a model whose rotary table has {target.max_pos}")
+    if temperature > 0:
+        u = torch.as_tensor([] if u is None else u, dtype=torch.float32)
+        if u.dim() != 2 or u.shape[0] < B or u.shape[1] < n_new:
+            raise ValueError(f"expected uniforms [{B}][{n_new}] at least, got {list(u.shape)}")
     keep_first = min(keep_first, budget)
     keep_recent = min(keep_recent or (budget - keep_first) // 2, budget - keep_first)
     limit = budget + page_size                                        # where a sequence is brought back to its budget
@@ -96,7 +100,7 @@ def budgeted_generate(target: Model, prompts, n_new: int, temperature: float, bu
     tokens[0] = torch.tensor([p[-1] for p in prompts], dtype=torch.int32, device=dev)
     logits = torch.empty((B, 1, V), dtype=torch.float32, device=dev)
     none = torch.empty(B, dtype=torch.int32, device=dev)
-    uniforms = torch.as_tensor(u, dtype=torch.float32).to(dev) if temperature > 0 else None
+    uniforms = u.to(dev) if temperature > 0 else None
     torch.cuda.synchronize()
     t0 = time.perf_counter()
     for i in range(n_new):

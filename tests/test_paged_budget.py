@@ -20,3 +20,10 @@ def test_generations_behind_the_rotary_table():
     for n, n_new in ((1, 65), (60, 6), (65, 1), (66, 0), (400, 40)):
         with pytest.raises(ValueError, match="rotary"):
             budgeted_generate(TARGET, [[1, 2], [3] * n], n_new, 0.0, 8)
+
+
+def test_uniforms_that_do_not_cover_the_batch():
+    """The acceptance kernel reads one of every sequence a step."""
+    for u in (None, [[0.5] * 4], [[0.5] * 3] * 2, [0.5] * 8):
+        with pytest.raises(ValueError, match="uniforms"):
+            budgeted_generate(TARGET, [[1, 2], [3]], 4, 0.8, 8, u=u)
