@@ -471,7 +471,8 @@ int ss_speculative_step_batched(ss_model *target, ss_kv_cache *target_kv, ss_mod
  * position received so far and its position in the sequence; eviction needs both.
  * What only the device sees is checked there: a page outside [0, n_pages) is neither read nor written, its positions are
  * masked (bit 3 of *status); positions beyond the table or the call's max_len are dropped (bit 4).  status may be NULL.
- * Sequences may have pages in common as long as no call writes them: appends, weights that are added up in place, evictions. */
+ * Sequences may have pages in common as long as no call writes them: appends, weights that are added up (in place or in an array apart: every
+ * sequence writes its own sum for the page), evictions. */
 typedef struct {
     void *k, *v;           /* dev, storage type */
     int64_t layer_stride, page_stride, head_stride, slot_stride;
@@ -495,12 +496,14 @@ int ss_paged_advance(const ss_paged_kv *kv, int32_t M, ss_stream stream);
 
 /* Attention of M rows per sequence (1 <= M <= 16; one: decoding; more: a verify pass, a chunk of a prompt) over the pages of one
  * layer: with n = len[b] + pending (pending: rows appended since the lengths moved last, usually M), row m sees the slots
- * 0 .. n - M + m.  out[r][h] = sum over them of softmax(scale * q[r][h] . k) v.  A row that sees nothing, or only scores of minus
+ * 0 .. n - M + m.  (Of a sequence that is cut, bit 4 of *status, n is what is left: the call's rows stand at the cut.)  out[r][h] = sum over them of softmax(scale * q[r][h] . k) v.  A row that sees nothing, or only scores of minus
  * infinity, is zero; what hidden places hold is of no influence, whatever it is; a score of NaN or plus
- * infinity makes its row's output NaN, an infinite or NaN value makes the elements that it belongs to infinite or NaN.
+ * infinity makes its row's output NaN, an infinite or NaN value makes the elements that it belongs to infinite or NaN.  scale: finite, and so
+ * log2(e) times it.
  * q_dev, out_dev: storage type, row r = b * M + m of head h at r * ld + h * head (elements); multiples of 16 bytes.  n_heads / n_kv_heads * M at most 1024.
  * weight_out_dev: NULL, or fp32 of weight's shape, which may be kv->weight: every position that n covers receives its weight
- * plus the sum of the softmax weights that the call's rows and the heads that share its key head gave it.
+ * plus the sum of the softmax weights that the call's rows and the heads that share its key head gave it (a row of NaN: NaN, and nothing to
+ * what it does not see).
  * max_len: the host's bound on n (0: what the table holds); the closer, the better the work is split.
  * ws_dev: ss_paged_attention_workspace_bytes bytes of scratch, 256-byte aligned, of one call at a time; needs no clearing. */
 size_t ss_paged_attention_workspace_bytes(const ss_paged_kv *kv, int32_t n_heads, int32_t M, int32_t max_len, int32_t weights);
@@ -525,7 +528,9 @@ int ss_paged_evict(const ss_paged_kv *kv, int32_t budget, int32_t keep_first, in
  * rotary table go through the decoder layers, are appended to the pages, and attend what these hold (weights != 0: and add what every
  * position received to kv->weight); then the lengths move.  The cache has the model's head shape and type (n_kv_heads = n_heads) and at
  * least its layers.  logits_dev fp32 [batch][M][vocab] or NULL; rows of idle places mean nothing.  A position that the model's rotary
- * table lacks is brought into it and sets bit 4 of kv->status.  One launch per phase, whatever ss_model_set_persistent says. */
+ * table lacks is brought into it and sets bit 4 of kv->status.  One launch per phase, whatever ss_model_set_persistent says.
+ * No call takes rows out of the pages again.  Behind a verify pass whose last rows were rejected the caller may set len and next_pos back: those slots are
+ * written anew, with a weight of zero.  What the rejected rows added to the weights of other positions stays; a pass with weights 0 adds nothing. */
 size_t ss_paged_forward_workspace_bytes(const ss_model *model, const ss_paged_kv *kv, int32_t M, int32_t max_len, int32_t weights);
 int ss_paged_forward(ss_model *model, const ss_paged_kv *kv, const int32_t *tokens_dev, int32_t M, int32_t weights, int32_t max_len,
                      float *logits_dev, void *ws_dev, size_t ws_bytes, ss_stream stream);

@@ -651,7 +651,8 @@ class PagedKV:
     k, v: [n_layers, n_pages, n_kv_heads, page_size, head_dim], fp32 or bf16, any strides but of the last dimension (equal for both),
     so [n_layers, n_pages, page_size, n_kv_heads, head_dim] transposed does as well.  page_table int32 [batch, max_pages]; length,
     next_pos int32 [batch]; weight fp32, position int32 [n_layers, n_pages, n_kv_heads, page_size]; status int32 [1].  The tensors'
-    contents are read on the device when a call runs; replace a tensor by making a new object."""
+    contents are read on the device when a call runs; replace a tensor by making a new object.  Calls without ws= take turns on the scratch that is kept
+    for their stream, whatever threads they come from; the tensors are the caller's to guard."""
 
     def __init__(self, k, v, page_table, length, next_pos=None, weight=None, position=None, status=None):
         if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in (torch.float32, torch.bfloat16):

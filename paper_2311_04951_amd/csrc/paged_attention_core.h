@@ -273,8 +273,9 @@ template <int N, int ALL, int SOME> __device__ __forceinline__ void wait_behind(
 // inside a head goes to the partials, 2 w for a part's first piece and 2 w + 1 for a last one that starts its head, and paged_join_kernel joins.
 //
 // One token over 200000 positions of 8 key heads reads 819 MB in 124 us (6.6 TB/s, with the join 128): the memory bounds it, and so it does any call of
-// one tile of rows over more than some ten megabytes.  With weights 8 x 9 rows at 4105 positions (548 MB) take 107 + 13 us, without 92.  Two tiles of
-// rows are bound by vector instructions: 16 rows of 16 x 8 heads at 4 x 3000 positions 55 us without weights, 0.34 PFLOP/s of products.
+// one tile of rows over more than some ten megabytes.  With weights 8 x 9 rows at 4105 positions (548 MB) take 108 + 13 us, without 90.  Two tiles of
+// rows are bound by vector instructions in bf16 and by the matrix instructions in fp32: 16 rows of 16 x 8 heads at 4 x 3000 positions 50 us without weights,
+// 0.38 PFLOP/s of products (hi and lo), matrix units busy a sixth of the time; in fp32 129 us, 98 TFLOP/s, busy 70 % of the time.
 template <typename T, int HD, int RT, int QP, bool WHOLE, bool W>
 __global__ __launch_bounds__(ATTN_WAVES * 64) void paged_attn_kernel(PagedAttnArgs a) {
     typedef PagedShape<T, HD> S;
